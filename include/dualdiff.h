@@ -273,7 +273,8 @@ int dd_cache_append(const void *k, const dd_strides *k_strides, const void *v, c
  *     out[b,h,i,:] = sum_j softmax_j(scale * q[b,h,i,:] . K_j) V_j
  * over the positions j < kv_len[b] (clamped to the table) whose page is there; K_j and V_j are the numbers that the cache's bytes
  * and scales (any that are finite and not negative) stand for.  No such position: out = 0.  Bytes of a page at and beyond
- * kv_len[b] are not looked at, NaN or not.  Scores, softmax and sums are fp32.  A query row enters the first product to 2^-18 of its
+ * kv_len[b] are not looked at, NaN or not, nor is anything of a page that begins there, whatever the table has for it.
+ * Scores, softmax and sums are fp32.  A query row enters the first product to 2^-18 of its
  * largest entry (bf16's own eight bits down to 2^-10 of that); a weight, times its values' scale, enters the second one to 2^-9 of itself and
  * 2^-27 of its row's largest weight and scale so far.  The result is rounded to bf16 once.  A row of q with an infinite or NaN
  * entry gives NaN.

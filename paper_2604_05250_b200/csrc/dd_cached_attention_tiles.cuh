@@ -110,10 +110,12 @@ __device__ __forceinline__ void copy_tiles(const CachedParams &p, const CUtensor
     const int pages = kTileKeys >> p.page_log2;          // of a tile: 1 to 8
     const int zero_row = p.num_pages * p.Hkv * p.page;   // beyond the pool: reads as zero
     Cursor ahead = now;                                  // the tile whose page numbers are under way
+    // A page that begins at or behind the sequence's end counts as one that is not there, whatever the table has for it: it may be given out
+    // ahead or be another sequence's, and its scales must not enter the tile's largest.
     auto fetch_ids = [&](const Cursor &c) {
         if (c.c >= c.end || lane >= pages) return -1;
         const int at = c.c * pages + lane;
-        return at < p.max_pages ? __ldg(p.table + (size_t)c.b * p.max_pages + at) : -1;
+        return (unsigned)at << p.page_log2 < (unsigned)c.keys ? __ldg(p.table + (size_t)c.b * p.max_pages + at) : -1;
     };
     auto step = [&] {
         if (++ahead.c < ahead.end || ahead.left == 0) return;

@@ -1,0 +1,56 @@
+"""dd_cached_attention: which scales of pages it may look at, and the range of those that it does."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_cached_attention import check, dd, make  # noqa: F401  (dd: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def reserve(s, page, how, scale):
+    """Valid entries in the table behind every sequence's last page: pages of their own, whose bytes are NaN and whose scales are
+    `scale`, or page 0 (padding), which gets such scales where it holds nobody's tokens."""
+    table, total = s["table_np"].copy(), s["cache"][0].shape[0]
+    used = {int(p) for b, n in enumerate(s["lens_np"]) for p in table[b, :-(-n // page)]}
+    behind = [(b, p) for b, n in enumerate(s["lens_np"]) for p in range(-(-n // page), table.shape[1])]
+    spare = [p for p in range(total) if p not in used]
+    for i, (b, p) in enumerate(behind):
+        table[b, p] = spare[i % len(spare)] if how == "spare" else 0
+    cache = [c.clone() for c in s["cache"]]
+    for p in spare:
+        for c in cache[2:]:
+            c[p] = scale
+    return tuple(cache), torch.from_numpy(table).cuda()
+
+
+@pytest.mark.parametrize("Nq", [1, 20, 40])
+@pytest.mark.parametrize("page", [16, 32, 64])
+@pytest.mark.parametrize("how", ["spare", "padded"])
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** 24, 2.0 ** 60, float("inf"), float("nan")])
+def test_pages_behind_the_end_are_not_looked_at(dd, Nq, page, how, scale):  # noqa: F811
+    """Pages given out ahead, and padding: bit for bit what a table without them gives, whatever stands in them."""
+    s = make(Nq + page, [1, 15, 17, 40, 65, 100, 129, 300, 0], 2, 2 if Nq == 1 else 1, Nq, 128 if page < 64 else 64, page, extra_pages=8)
+    want = check(dd, s)
+    cache, table = reserve(s, page, how, scale)
+    got = dd.cached_attention(s["q"], dd.Cache(*cache), table, s["lens"])
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("Nq", [1, 40])
+def test_a_page_that_held_infinity_and_is_reserved(dd, Nq):  # noqa: F811
+    """An append of an infinite value leaves a scale of 2^60; its page, given to another sequence for later, changes nothing there."""
+    heads, D, page = 2, 128, 32
+    g = torch.Generator(device="cuda").manual_seed(3)
+    cache = dd.new_cache(4, heads, page, D)
+    as_int = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    k, v = (torch.randn(1, 50, heads, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn(1, Nq, heads, D, generator=g, device="cuda").bfloat16()
+    dd.cache_append(k, v, cache, as_int(0, 1).view(1, 2), as_int(0))
+    want = dd.cached_attention(q, cache, as_int(0, 1, -1).view(1, 3), as_int(50))
+    bad = v[:, :1].clone()
+    bad[..., 0] = float("inf")
+    dd.cache_append(k[:, :1], bad, cache, as_int(2).view(1, 1), as_int(0))
+    assert float(cache.v_scale[2, 0]) == 2.0 ** 60
+    got = dd.cached_attention(q, cache, as_int(0, 1, 2).view(1, 3), as_int(50))
+    assert want.abs().max() > 0.1 and torch.equal(got, want)
