@@ -258,8 +258,9 @@ cached_attention_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const _
                     s[j] = y.x; s[j + 1] = y.y;
                     over = max3(over, y.x, y.y);
                 }
+                // (a column without a reference point, its tiles so far having no key, takes one with the first key: its sum must not start at 0)
                 const bool first = c == now.c0, grows = vmax > 0.f && (!any_far || vmax > far);
-                if (any_of_128(barrier, there && over > kNarrowLag) || first || grows) {
+                if (any_of_128(barrier, there && (over > kNarrowLag || m_col == -INFINITY)) || first || grows) {
                     // ---- the reference points (s is relative to the old ones)
                     float shrink = 1.f;
                     if (grows) {

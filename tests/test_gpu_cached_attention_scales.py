@@ -54,3 +54,18 @@ def test_a_page_that_held_infinity_and_is_reserved(dd, Nq):  # noqa: F811
     assert float(cache.v_scale[2, 0]) == 2.0 ** 60
     got = dd.cached_attention(q, cache, as_int(0, 1, 2).view(1, 3), as_int(50))
     assert want.abs().max() > 0.1 and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("Nq", [1, 20, 40])
+@pytest.mark.parametrize("page", [16, 64, 128])
+def test_values_of_zero_scale_behind_missing_pages(dd, Nq, page):  # noqa: F811
+    """The first tile's pages are not there, the next one's values stand under scales of zero: its keys count all the same, whether a
+    positive scale follows (in the same share or in another) or not."""
+    lens, heads = [500, 256, 390, 300] * 12, 8
+    per = 128 // page
+    s = make(page + Nq, lens, heads, 1, Nq, 64, page, strength=0.01, missing=[(b, p) for b in range(len(lens)) for p in range(per)])
+    for b in range(len(lens)):
+        for p in range(per, 2 * per):
+            s["scales"][1][s["table_np"][b, p]] = 0.0
+            s["cache"][3][s["table_np"][b, p]] = 0.0
+    check(dd, s)
