@@ -241,7 +241,7 @@ int dd_qk_norm_rope(const void *q, const dd_strides *q_strides, int H, const voi
  */
 typedef struct {
     void *k, *v;                /* [num_pages, heads, page_size, D] e4m3 bytes, contiguous, 16-byte aligned       */
-    float *k_scale, *v_scale;   /* [num_pages, heads] fp32                                                      */
+    float *k_scale, *v_scale;   /* [num_pages, heads] fp32; of pages that hold tokens 0 to 2^100                 */
     const int32_t *page_table;  /* [B, max_pages]                                                               */
     int num_pages, max_pages;
     int page_size;              /* 16, 32, 64 or 128                                                            */
@@ -272,12 +272,12 @@ int dd_cache_append(const void *k, const dd_strides *k_strides, const void *v, c
  * h / (H / cache->heads),
  *     out[b,h,i,:] = sum_j softmax_j(scale * q[b,h,i,:] . K_j) V_j
  * over the positions j < kv_len[b] (clamped to the table) whose page is there; K_j and V_j are the numbers that the cache's bytes
- * and scales (any that are finite and not negative) stand for.  No such position: out = 0.  Bytes of a page at and beyond
+ * and scales (any from 0 to 2^100, powers of two or not) stand for.  No such position: out = 0.  Bytes of a page at and beyond
  * kv_len[b] are not looked at, NaN or not, nor is anything of a page that begins there, whatever the table has for it.
- * Scores, softmax and sums are fp32.  A query row enters the first product to 2^-18 of its
+ * Scores, softmax and sums are fp32; the result is finite for |V_j| * kv_len[b] < 2^100.  A query row enters the first product to 2^-18 of its
  * largest entry (bf16's own eight bits down to 2^-10 of that); a weight, times its values' scale, enters the second one to 2^-9 of itself and
- * 2^-27 of its row's largest weight and scale so far.  The result is rounded to bf16 once.  A row of q with an infinite or NaN
- * entry gives NaN.
+ * 2^-27 of its row's largest weight and scale so far (of that weight and 2^-100 where all scales so far are smaller).  The result is
+ * rounded to bf16 once.  A row of q with an infinite or NaN entry gives NaN.
  * q: bf16 [B,Nq,H,D], any strides (DD_LAYOUT_BHND is a choice of strides), 16-byte aligned; out: bf16 with strides likewise, rows not
  * overlapping one another or the inputs; kv_len: int32 [B] DEVICE pointer.
  * workspace: device memory of dd_cached_attention_workspace_bytes() bytes or more, 16-byte aligned, that no other call uses until

@@ -19,7 +19,7 @@
 // Queries: a row is taken under a power of two that brings its largest entry into (224, 448]; two e4m3 numbers then hold bf16's eight bits
 // exactly down to 2^-10 of the row's largest entry, and are within 2^-18 of that for smaller ones.
 // Weights are relative to a reference point of the row that may lag its maximum by a factor of 2^5, times the values' scales (relative to
-// a power of two no smaller than any so far), times 2^10: three e5m2 numbers are within 2^-9 of a weight (half a step of bf16),
+// a power of two no smaller than any so far, of 2^-100 to 2^100: the range of scales), times 2^10: three e5m2 numbers are within 2^-9 of a weight (half a step of bf16),
 // and what is lost below their smallest step is at most 2^-27 of the reference's weight.
 // A row's maximum is spread over the lanes here, but as long as no weight outgrows the lag it is not needed: the warps agree
 // on that by one barrier with a vote, and only where the vote fails (the first tile, and rarely later) the maxima are gathered.

@@ -16,7 +16,7 @@
 // the sum of two e4m3 numbers an entry: bf16's eight bits exactly down to 2^-10 of the row's largest entry, and within 2^-18 of that
 // for smaller ones.  Twice the products at twice the rate of f16, and no keys to convert.
 // Weights relative to a reference point of the row that may lag the row's maximum by a factor of 2^6, times the values' scales (relative to
-// a power of two no smaller than any so far), in f16 with 2^8 on top: nothing overflows, and what underflows is below 2^-32 of the reference.
+// a power of two no smaller than any so far, of 2^-100 to 2^100: the range of scales), in f16 with 2^8 on top: nothing overflows, and what underflows is below 2^-32 of the reference.
 //
 // Included by dd_cached_attention.cu (inside its unnamed namespace).
 #pragma once

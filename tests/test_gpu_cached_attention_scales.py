@@ -69,3 +69,43 @@ def test_values_of_zero_scale_behind_missing_pages(dd, Nq, page):  # noqa: F811
             s["scales"][1][s["table_np"][b, p]] = 0.0
             s["cache"][3][s["table_np"][b, p]] = 0.0
     check(dd, s)
+
+
+@pytest.mark.parametrize("Nq", [1, 20, 40])
+@pytest.mark.parametrize("low,high", [(-100, -96), (-60, -40), (40, 60), (70, 76), (-100, 76)])
+def test_range_of_scales(dd, Nq, low, high):  # noqa: F811
+    """Values under very small and very large scales (numbers below 2^100 / kv_len), and keys under as small ones."""
+    s = make(Nq + high + 100, [300, 70], 2, 2, Nq, 128, 16)
+    g = np.random.default_rng(low + high + 200)
+    s["scales"][1][:] = 2.0 ** g.integers(low, high + 1, size=s["scales"][1].shape)
+    s["cache"][3][:] = torch.from_numpy(s["scales"][1]).float().cuda()
+    if high < 0:
+        s["scales"][0][:] = 2.0 ** g.integers(low, high + 1, size=s["scales"][0].shape)
+        s["cache"][2][:] = torch.from_numpy(s["scales"][0]).float().cuda()
+    check(dd, s)
+
+
+@pytest.mark.parametrize("Nq", [1, 40])
+def test_values_of_zero_under_the_largest_scale(dd, Nq):  # noqa: F811
+    s = make(Nq, [300], 2, 1, Nq, 128, 64)
+    page = int(s["table_np"][0, 1])
+    s["pools"][1][page] = 0.0
+    s["cache"][1].view(torch.uint8)[page] = 0
+    s["scales"][1][page] = 2.0 ** 100
+    s["cache"][3][page] = 2.0 ** 100
+    got = dd.cached_attention(s["q"], dd.Cache(*s["cache"]), s["table"], s["lens"])
+    assert got.isfinite().all()
+
+
+@pytest.mark.parametrize("Nq", [1, 20, 40])
+@pytest.mark.parametrize("by", [-93, -50, 50, 93])
+def test_scales_times_a_power_of_two(dd, Nq, by):  # noqa: F811
+    """The same bits under another exponent, from 2^-100 to 2^100."""
+    s = make(Nq, [300, 70, 1], 2, 2, Nq, 128, 32)          # scales of 2^-11 to 2^-5
+    s["cache"][3].mul_(2.0 ** 4)                             # 2^-7 to 2^-1
+    if by > 0:
+        s["cache"][3].mul_(2.0 ** 8)                         # 2 to 2^7
+    cache = dd.Cache(*s["cache"])
+    want = dd.cached_attention(s["q"], cache, s["table"], s["lens"])
+    got = dd.cached_attention(s["q"], cache._replace(v_scale=cache.v_scale * 2.0 ** by), s["table"], s["lens"])
+    assert torch.equal(got.double(), want.double() * 2.0 ** by)
