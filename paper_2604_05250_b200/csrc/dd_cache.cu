@@ -102,7 +102,7 @@ struct AppendParams {
     int B, N, H, num_pages, max_pages, page_log2, touched;
 };
 
-constexpr int kScaleLow = -60, kScaleHigh = 60;
+constexpr int kScaleLow = -60, kScaleHigh = 60, kHeldHigh = 100;       // of the scales made here, and of those that a cache may hold
 
 // Smallest e with x <= 448 * 2^e = 1.75 * 2^(e + 8), for finite x >= 0; within the range of scales.
 __device__ __forceinline__ int scale_exponent(float x)
@@ -117,7 +117,7 @@ __device__ __forceinline__ int held_exponent(float x)
     const uint32_t u = __float_as_uint(x);
     if (!(x > 0.f)) return kScaleLow;
     const int e = (int)(u >> 23) - 127 + ((u & 0x7FFFFFu) != 0);
-    return max(kScaleLow, min(kScaleHigh, e));
+    return max(kScaleLow, min(kHeldHigh, e));
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 

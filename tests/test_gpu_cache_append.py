@@ -210,6 +210,16 @@ def test_append_scales_that_are_no_powers_of_two(dd):
     run_append(dd, raw, table, rows(g, 2, 4, 2, 128), rows(g, 2, 4, 2, 128), [5, 40], kv_len=[20, 40])
 
 
+@pytest.mark.parametrize("page", [16, 128])
+def test_append_to_pages_under_large_scales(dd, page):
+    """Scales beyond those that an append makes (a cache quantised elsewhere) stay where tokens of the page stay."""
+    g = np.random.default_rng(page)
+    table, raw = state(21, 2, 2, page, 64, 2)
+    raw = [(x, torch.from_numpy(2.0 ** g.choice([-100, -61, 60, 61, 62, 75, 100], size=tuple(s.shape))).float()) for x, s in raw]
+    raw = [(x, s * (1 + 0.5 * torch.from_numpy(g.integers(0, 2, size=tuple(s.shape))).float() * (s < 2.0 ** 99))) for x, s in raw]
+    run_append(dd, raw, table, rows(g, 2, 4, 2, 64), rows(g, 2, 4, 2, 64), [5, 9], kv_len=[12, 14])
+
+
 def test_append_again_changes_nothing(dd):
     g = np.random.default_rng(13)
     table, raw = state(14, 3, 2, 64, 128, 3)
