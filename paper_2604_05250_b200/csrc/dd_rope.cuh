@@ -5,8 +5,9 @@
 //   (i, i + dims/2), or neighbours (2i, 2i + 1); the angle of pair i at a position is entry i of that position's row in the tables.
 //
 // D / 16 lanes hold a row, each two chunks of 8 entries (16 bytes of bf16): the two members of a pair are then always in one lane,
-// whichever the pairing, and a lane's 8 pairs take 8 neighbouring entries of the tables.  All arithmetic is fp32 and in the order
-// written here, every product rounded by itself (no contraction), so that a row's result does not depend on which kernel computes it.
+// whichever the pairing, and a lane's 8 pairs take 8 neighbouring entries of the tables.  All arithmetic is fp32, in the order and with the
+// roundings written here (fused where it says so, each product by itself elsewhere; nothing is left to the compiler's contraction), so that
+// a row's result does not depend on which kernel computes it.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -94,11 +95,11 @@ __device__ __forceinline__ void norm_rows(float (&x)[16], const __nv_bfloat16 *w
     if (!any) return;
     float ss = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) ss += x[i] * x[i];
+    for (int i = 0; i < 16; ++i) ss = __fmaf_rn(x[i], x[i], ss);
 #pragma unroll
-    for (int o = Lane<D>::kLanes / 2; o > 0; o /= 2) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+    for (int o = Lane<D>::kLanes / 2; o > 0; o /= 2) ss = __fadd_rn(ss, __shfl_xor_sync(0xFFFFFFFFu, ss, o));
     if (!weight) return;
-    const float r = rsqrtf(ss * (1.f / D) + eps);
+    const float r = rsqrtf(__fmaf_rn(ss, 1.f / D, eps));
     float w[16];
     unpack<kMixed>(w, __ldg(reinterpret_cast<const uint4 *>(weight) + l.a));
     unpack<kMixed>(w + 8, __ldg(reinterpret_cast<const uint4 *>(weight) + l.b));

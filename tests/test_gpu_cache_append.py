@@ -220,6 +220,38 @@ def test_append_to_pages_under_large_scales(dd, page):
     run_append(dd, raw, table, rows(g, 2, 4, 2, 64), rows(g, 2, 4, 2, 64), [5, 9], kv_len=[12, 14])
 
 
+@pytest.mark.parametrize("D,dims,interleaved", [(64, 64, False), (128, 128, False), (128, 64, True), (128, 0, False)])
+def test_a_row_is_the_same_whoever_computes_it(dd, D, dims, interleaved):
+    """Norm and rotation in a call of one token, of many, and on the way into a cache: the same 32-bit numbers, so the same roundings."""
+    g = np.random.default_rng(D + dims)
+    B, N, heads, page = 2, 700, 6, 64
+    k, w = rows(g, B, N, heads, D, spread=2).cuda(), weight_of(g, D).cuda()
+    cos, sin = (t.cuda() for t in angles(N, dims)) if dims else (None, None)
+    call = lambda x, at: dd.qk_norm_rope(x, q_weight=w, eps=EPS, cos=cos, sin=sin, interleaved=interleaved,  # noqa: E731
+                                         start=torch.full((B,), at, dtype=torch.int32, device="cuda"))[0]
+    many = call(k, 0)
+    for i in range(0, N, 50):
+        assert torch.equal(call(k[:, i:i + 1], i), many[:, i:i + 1])
+    # into a cache: the e4m3 numbers next to the 32-bit results are those next to the bf16 ones, where these are not half-way between two
+    wide = -(-N // page)
+    table = torch.arange(B * wide, dtype=torch.int32, device="cuda").view(B, wide)
+    at = torch.zeros(B, dtype=torch.int32, device="cuda")
+    whole = dd.cache_append(k, k, dd.new_cache(B * wide, heads, page, D), table, at, k_weight=w, eps=EPS, cos=cos, sin=sin, interleaved=interleaved)
+    single = dd.new_cache(B * wide, heads, page, D)
+    for i in range(N):
+        dd.cache_append(k[:, i:i + 1], k[:, i:i + 1], single, table, at + i, k_weight=w, eps=EPS, cos=cos, sin=sin, interleaved=interleaved)
+    assert torch.equal(whole.k_scale, single.k_scale) and torch.equal(whole.v_scale, single.v_scale)
+    order = lambda x: x.float().view(B, wide, heads, page, D).transpose(2, 3).reshape(B, wide * page, heads, D)[:, :N].double().cpu().numpy()  # noqa: E731
+    scale = whole.k_scale.view(B, wide, 1, heads, 1).expand(B, wide, page, heads, 1).reshape(B, wide * page, heads, 1)[:, :N].double().cpu().numpy()
+    x = many.double().cpu().numpy() / scale
+    got = order(whole.k)
+    lower, upper = ref.to_e4m3(x * (1 - 2.0 ** -8)), ref.to_e4m3(x * (1 + 2.0 ** -8))
+    sure = lower == upper
+    assert sure.mean() > 0.8 and (got[sure] == lower[sure]).all()
+    middle = (x != 0) & (np.abs(x) < 448) & (ref.to_e4m3(x * (1 - 2.0 ** -20)) != ref.to_e4m3(x * (1 + 2.0 ** -20)))
+    assert (got[~middle] == ref.to_e4m3(x)[~middle]).all()
+
+
 def test_append_again_changes_nothing(dd):
     g = np.random.default_rng(13)
     table, raw = state(14, 3, 2, 64, 128, 3)
