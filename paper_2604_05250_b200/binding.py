@@ -52,7 +52,8 @@ class _Cache(ctypes.Structure):
 
 class Cache(NamedTuple):
     """The pools of a paged 8-bit cache of one layer (dd_cache): k, v torch.float8_e4m3fn [num_pages, heads, page_size, D],
-    k_scale, v_scale torch.float32 [num_pages, heads].  new_cache() makes one; pages are the caller's to give out."""
+    k_scale, v_scale torch.float32 [num_pages, heads].  new_cache() makes one; pages are the caller's to give out.  The calls take a
+    plain tuple of the four tensors as well."""
     k: Tensor
     v: Tensor
     k_scale: Tensor
@@ -468,6 +469,13 @@ def _rotation(cos, sin, interleaved, like):
 
 
 def _cache_view(cache, page_table, B, like):
+    if not isinstance(cache, tuple) or len(cache) != 4:
+        raise TypeError("cache: expected a Cache (k, v, k_scale, v_scale)")
+    cache = Cache(*cache)
+    if not isinstance(cache.k, Tensor):
+        raise TypeError("cache.k: expected a torch.Tensor")
+    if cache.k.dim() != 4:
+        raise ValueError(f"cache.k: expected [num_pages, heads, page_size, D], got {tuple(cache.k.shape)}")
     num_pages, heads, page, D = shape = tuple(cache.k.shape)
     _require(cache.k, _E4M3, shape, True, "cache.k")
     _require(cache.v, _E4M3, shape, True, "cache.v")

@@ -105,6 +105,25 @@ def test_binding_words_what_it_refuses(dd):
         dd.cached_attention(q, c._replace(k=_on_device(c.k), v=c.v.float()), table, None)
 
 
+def test_binding_takes_a_tuple_as_a_cache_and_nothing_else(dd):
+    """Four tensors in a plain tuple are a cache, as for the native host side; other things are refused in words."""
+    q, table, start = torch.zeros(1, 4, 2, 64, dtype=torch.bfloat16), torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    c = tuple(dd.new_cache(3, 2, 16, 64, device="cpu"))
+    with pytest.raises(ValueError, match="cache.k: expected a device tensor"):
+        dd.cache_append(q, q, c, table, start)
+    with pytest.raises(ValueError, match="cache.k: expected a device tensor"):
+        dd.cached_attention(q, c, table, start)
+    for bad in (None, c[:3], list(c), 7):
+        with pytest.raises(TypeError, match="cache: expected a Cache"):
+            dd.cache_append(q, q, bad, table, start)
+        with pytest.raises(TypeError, match="cache: expected a Cache"):
+            dd.cached_attention(q, bad, table, start)
+    with pytest.raises(TypeError, match="cache.k: expected a torch.Tensor"):
+        dd.cached_attention(q, (None, *c[1:]), table, start)
+    with pytest.raises(ValueError, match="cache.k: expected"):
+        dd.cached_attention(q, (c[0][0], *c[1:]), table, start)
+
+
 class _on_device(torch.Tensor):
     """A host tensor that says it is on the device: gets past the first check, to the next one."""
 
