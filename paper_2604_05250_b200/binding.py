@@ -8,6 +8,7 @@ missing the first call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib.util
 import os
@@ -213,6 +214,15 @@ def _stream_ptr(stream):
     return _raw_stream(_device())
 
 
+def _made_on(stream):
+    """Within this, outputs are made as memory of the stream that the call runs on, as torch's own operators make theirs: the current
+    stream's may still be read there.  (Whoever reads an output on another stream says so to torch, with Tensor.record_stream.)"""
+    if stream is None:
+        return contextlib.nullcontext()
+    # (anything with a cuda_stream will do: another library's stream)
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream))
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -248,7 +258,8 @@ def bidir_attention(q, k, v, out=None, scale=None, stream=None, host=False):
         for name, t in (("q", q), ("k", k), ("v", v)):
             _require(t, _BF16, (B, H, N, D), cuda, name)
     if out is None:
-        out = torch.empty_like(q)
+        with _made_on(stream):
+            out = torch.empty_like(q)
     elif not _fits(out, _BF16, shape, cuda):
         _require(out, _BF16, (B, H, N, D), cuda, "out")
     if scale is None:
@@ -292,7 +303,8 @@ def block_attention(q, k, v, kv_len=None, layout="bhnd", out=None, scale=None, s
     if kv_len is not None and not _fits(kv_len, _I32, (B,), True):
         _require(kv_len, _I32, (B,), True, "kv_len")
     if out is None:
-        out = torch.empty_like(q)
+        with _made_on(stream):
+            out = torch.empty_like(q)
     elif not _fits(out, _BF16, shape, True):
         _require(out, _BF16, tuple(shape), True, "out")
     if scale is None:
@@ -311,20 +323,21 @@ def _decision_inputs(tokens, mask_flags, shape, cuda):
         _require(mask_flags, _U8, shape, cuda, "mask_flags")
 
 
-def _decision_outputs(out_tokens, out_mask, out_score, want_score, tokens, mask_flags, like, shape, host, score_name):
-    """The three outputs of shape [B,P]: made where they are None, checked where they are given."""
+def _decision_outputs(out_tokens, out_mask, out_score, want_score, tokens, mask_flags, like, shape, host, score_name, stream):
+    """The three outputs of shape [B,P]: made where they are None (on the call's stream), checked where they are given."""
     cuda = not host
     near = cuda and tokens.device == like.device and mask_flags.device == like.device
 
     def make(source, dtype):
-        return torch.empty_like(source, dtype=dtype) if near else torch.empty(shape, dtype=dtype, device=like.device, pin_memory=host)
+        with _made_on(stream):
+            return torch.empty_like(source, dtype=dtype) if near else torch.empty(shape, dtype=dtype, device=like.device, pin_memory=host)
 
     if out_tokens is None:
-        out_tokens = torch.empty_like(tokens) if near else make(tokens, _I32)
+        out_tokens = make(tokens, _I32)
     elif not _fits(out_tokens, _I32, shape, cuda):
         _require(out_tokens, _I32, shape, cuda, "out_tokens")
     if out_mask is None:
-        out_mask = torch.empty_like(mask_flags) if near else make(mask_flags, _U8)
+        out_mask = make(mask_flags, _U8)
     elif not _fits(out_mask, _U8, shape, cuda):
         _require(out_mask, _U8, shape, cuda, "out_mask")
     if out_score is None:
@@ -358,7 +371,7 @@ def verify(drafter_logits, verifier_logits, tokens, mask_flags, mode, tau, k, se
     shape = (B, P)
     _decision_inputs(tokens, mask_flags, shape, cuda)
     out_tokens, out_mask, out_score = _decision_outputs(out_tokens, out_mask, out_score, want_score, tokens, mask_flags,
-                                                        verifier_logits, shape, host, "out_score")
+                                                        verifier_logits, shape, host, "out_score", stream)
     L = _lib or lib()
     fn = L.dd_verify_host if host else (L.dd_verify_static if static_scratch else L.dd_verify)
     status = fn(_ptr(drafter_logits), verifier_logits.data_ptr(), tokens.data_ptr(), mask_flags.data_ptr(),
@@ -387,7 +400,7 @@ def lm_head_verify(drafter_hidden, drafter_weight, verifier_hidden, verifier_wei
     shape = (B, P)
     _decision_inputs(tokens, mask_flags, shape, True)
     out_tokens, out_mask, out_score = _decision_outputs(out_tokens, out_mask, out_score, True, tokens, mask_flags,
-                                                        verifier_hidden, shape, False, "out_score")
+                                                        verifier_hidden, shape, False, "out_score", stream)
     status = (_lib or lib()).dd_lm_head_verify(
         _ptr(drafter_hidden), _ptr(drafter_weight), verifier_hidden.data_ptr(), verifier_weight.data_ptr(),
         tokens.data_ptr(), mask_flags.data_ptr(), int(mode), float(tau), int(k), int(seed) & 0xFFFFFFFFFFFFFFFF,
@@ -413,7 +426,7 @@ def unmask(logits, tokens, mask_flags, tau, k, out_tokens=None, out_mask=None, o
     shape = (B, P)
     _decision_inputs(tokens, mask_flags, shape, True)
     out_tokens, out_mask, out_conf = _decision_outputs(out_tokens, out_mask, out_conf, True, tokens, mask_flags,
-                                                       logits, shape, False, "out_conf")
+                                                       logits, shape, False, "out_conf", stream)
     status = (_lib or lib()).dd_unmask(logits.data_ptr(), tokens.data_ptr(), mask_flags.data_ptr(), float(tau), int(k),
                                        out_tokens.data_ptr(), out_mask.data_ptr(), out_conf.data_ptr(), B, P, V,
                                        _stream_ptr(stream))
@@ -443,8 +456,8 @@ def _one_device(like, **tensors):
 
 
 def _device_of(like, stream):
-    """The tensors' device is the current one within this context; a stream that is given has to be of that device."""
-    if stream is not None and stream.device != like.device:
+    """The tensors' device is the current one within this context; a stream that is given has to be of that device, if it says of which it is."""
+    if stream is not None and getattr(stream, "device", like.device) != like.device:
         raise ValueError(f"stream: on {stream.device}, the tensors are on {like.device}")
     return torch.cuda.device(like.device)
 
@@ -548,12 +561,12 @@ def qk_norm_rope(q, k=None, q_weight=None, k_weight=None, eps=1e-6, cos=None, si
         _one_device(q, **{name: given})
         return given
 
-    out_q = output(out_q, H, "out_q")
-    if k is not None:
-        out_k = output(out_k, Hkv, "out_k")
-    elif out_k is not None:
+    if k is None and out_k is not None:
         raise ValueError("out_k: given without k")
-    with _device_of(q, stream):
+    with _device_of(q, stream), _made_on(stream):
+        out_q = output(out_q, H, "out_q")
+        if k is not None:
+            out_k = output(out_k, Hkv, "out_k")
         status = (_lib or lib()).dd_qk_norm_rope(
             q.data_ptr(), ctypes.byref(_row_strides(q)), H, _ptr(k), None if k is None else ctypes.byref(_row_strides(k)), Hkv, wq, wk,
             float(eps), None if rotation is None else ctypes.byref(rotation), st, out_q.data_ptr(), _ptr(out_k), B, N, D, code,
@@ -625,9 +638,7 @@ def cached_attention(q, cache, page_table, kv_len, layout="bnhd", out=None, scal
     if kv_len is None:
         raise TypeError("kv_len: expected a torch.Tensor")
     lens = _lengths(kv_len, B, "kv_len", q)
-    if out is None:
-        out = torch.empty(q.shape, dtype=_BF16, device=q.device)
-    else:
+    if out is not None:
         _require_rows(out, q.shape, "out")
         _one_device(q, out=out)
         if any(n > 1 and s == 0 for n, s in zip(out.shape, out.stride())):
@@ -635,7 +646,9 @@ def cached_attention(q, cache, page_table, kv_len, layout="bnhd", out=None, scal
     if scale is None:
         scale = float(D) ** -0.5
     L = _lib or lib()
-    with _device_of(q, stream), torch.cuda.stream(stream):       # (the allocator then knows which stream the workspace is used on)
+    with _device_of(q, stream), _made_on(stream):                # (the workspace too)
+        if out is None:
+            out = torch.empty(q.shape, dtype=_BF16, device=q.device)
         need = L.dd_cached_attention_workspace_bytes(B, H, Nq, ctypes.byref(view))
         work = torch.empty(max(need, 16), dtype=_U8, device=q.device)
         status = L.dd_cached_attention(
