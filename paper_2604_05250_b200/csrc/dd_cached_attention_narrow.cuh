@@ -216,7 +216,9 @@ cached_attention_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const _
                 }
             }
             const int keys = now.keys;
-            float l[16], m_col = -INFINITY, far = 1.f;           // m_col: the reference point of column `lane` % 16
+            // m_col: the reference point of column `lane` % 16; limit: how far a score may be beyond its own.  As long as a column has none (its tiles
+            // so far had no key) any key calls for one: its sum must not begin at 0.
+            float l[16], m_col = -INFINITY, far = 1.f, limit = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 16; ++j) l[j] = 0.f;
             bool any_far = false;
@@ -258,9 +260,8 @@ cached_attention_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const _
                     s[j] = y.x; s[j + 1] = y.y;
                     over = max3(over, y.x, y.y);
                 }
-                // (a column without a reference point, its tiles so far having no key, takes one with the first key: its sum must not start at 0)
                 const bool first = c == now.c0, grows = vmax > 0.f && (!any_far || vmax > far);
-                if (any_of_128(barrier, there && (over > kNarrowLag || m_col == -INFINITY)) || first || grows) {
+                if (any_of_128(barrier, there && over > limit) || first || grows) {
                     // ---- the reference points (s is relative to the old ones)
                     float shrink = 1.f;
                     if (grows) {
@@ -280,6 +281,7 @@ cached_attention_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const _
                     const float old = m_col;
                     if (old == -INFINITY) m_col = rise;
                     else if (rise > kNarrowLag) m_col = old + rise;
+                    if (__all_sync(0xFFFFFFFFu, m_col != -INFINITY)) limit = kNarrowLag;
                     const float move = m_col == -INFINITY ? 0.f : old == -INFINITY ? m_col : m_col - old;
                     if (w4 == 0) {
                         sh.move[half][lane] = move;

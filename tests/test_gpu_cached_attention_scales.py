@@ -109,3 +109,14 @@ def test_scales_times_a_power_of_two(dd, Nq, by):  # noqa: F811
     want = dd.cached_attention(s["q"], cache, s["table"], s["lens"])
     got = dd.cached_attention(s["q"], cache._replace(v_scale=cache.v_scale * 2.0 ** by), s["table"], s["lens"])
     assert torch.equal(got.double(), want.double() * 2.0 ** by)
+
+
+def test_rows_that_are_not_finite_behind_missing_pages(dd):  # noqa: F811
+    """A row of NaN scores never gets a reference point; the rows beside it are the same as without it."""
+    s = make(31, [600, 300], 2, 1, 20, 128, 64, missing=[(0, 0), (0, 1), (1, 2)])
+    want = check(dd, s)
+    s["q"][:, 7, 1] = float("nan")
+    got = dd.cached_attention(s["q"], dd.Cache(*s["cache"]), s["table"], s["lens"])
+    assert got[:, 7, 1].isnan().all()
+    got[:, 7, 1] = want[:, 7, 1]
+    assert torch.equal(got, want)
