@@ -139,9 +139,10 @@ cached_attention_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const _
     Cursor now;
     const bool misplaced = base & 1023;                          // the swizzles go by the address
     if (misplaced && tid == 0) report(p, kErrPlace);
-    // (a wait that has expired before: nothing more is begun)
+    // (a wait that has expired before: nothing more is begun; one lane's word for the warp, whose lanes find their share together)
     const Split split(p, lane);
-    const bool work = __syncthreads_and(!misplaced && *reinterpret_cast<volatile unsigned int *>(p.status) == 0 && find_share(p, lane, split, now));
+    const bool quiet = warp_uniform(*reinterpret_cast<volatile unsigned int *>(p.status)) == 0;
+    const bool work = __syncthreads_and(!misplaced && quiet && find_share(p, lane, split, now));
     clear_empty<D>(p);
     if (!work) {
         if (tid == 0) write_record<D>(p, split, now, false);
