@@ -91,6 +91,7 @@ __device__ __forceinline__ uint32_t half2_bits(float a, float b)
 // How the chunks of all items (in order, an item's in the keys' order) are shared out, found by each warp for itself, no barrier.
 // Shares of equal cost, across items, where an item costs its chunks and kEnds more at its front for its start and end.
 // 16 x 32 heads, 32 queries over up to 1024 keys (CTAs with one to four items) 45 us without that cost, 36 with it; of 1, 2 and 3 the best was 2.
+// Where tiles are no more than CTAs, that cost leaves some CTAs without a tile and others with two (51 of 256 each for 32 items of 8 tiles).
 // (Items cut into parts of equal length, a CTA each, where that makes none longer: 0.2 us less for one shape, 0.3 to 4 more for fourteen others.)
 struct Split {
     static constexpr unsigned kEnds = 2;

@@ -14,7 +14,8 @@
 // What bounds it (D = 128, a graph's replays): bytes for long caches, one token of 16 sequences of up to 16384 keys, 32 heads on 8, 57 us, 6.07
 // TB/s, 0.93 of what a copy reaches; for 32 rows of shorter ones a CTA's ends and the softmax's instructions, 16 x 32 heads, 32
 // queries over up to 1024 keys 35 us, 2.7 TB/s (IPC 2.1, ALU pipe 42 %, two items a CTA); for few keys the chain of latencies from the lengths
-// to the joined result, one token of one sequence of 1024 keys, 32 heads, 9.6 us, of 64 keys (no join to wait for) 6.8.
+// to the joined result, one token of one sequence of 1024 keys, 32 heads, 9.6 us, of 64 keys (nothing to join) 7.0.
+// At 80 registers a thread the form for 32 rows spills 192 bytes, the form for 16 (128 registers) none.
 //
 // Queries: a row is taken under a power of two that brings its largest entry into (224, 448]; two e4m3 numbers then hold bf16's eight bits
 // exactly down to 2^-10 of the row's largest entry, and are within 2^-18 of that for smaller ones.

@@ -9,6 +9,7 @@
 // next scores wait for its products; a tile takes a CTA alone 2.2 us and two of them 1.6 us of the SM, of which the tensor core works 0.55 and
 // the exponentials' unit 0.54.  8 x 32 heads, 256 queries over 8192 keys 333 us (826 TFLOP/s of the definition's products, 0.50 of what a
 // library's bf16 product reaches); 2 x 32 heads over 4096 keys 60 us, of which some 15 are the ends: share, queries, result, join.
+// At 80 registers a thread it spills 196 bytes.
 // A row's weights taken before its largest score is known, and anew where they turn out too large: 301 us if none ever did, but 432 with
 // heads as peaked as these (scores of a deviation of 8), where some row of 128 outgrows its reference point in most tiles.
 //
